@@ -445,7 +445,7 @@ __global__ __launch_bounds__(kRecMaxThreads, 4) void recurrence_bwd_kernel(RecPa
       const float now = fmaf(f[i][k], s[k], u[i][k] * c[k]);
       dr[k] = ds[i][k] * now;
       ds[i][k] = (s[k] - c[k]) * (f[i][k] * u[i][k]);
-      sum[2][k] += dr[k];
+      sum[2][k] += i < rows ? dr[k] : 0.f;   // (behind the last token zero times the state, which may be infinite)
       (k ? state.y : state.x) = now;
     }
     here(ds[i]);
@@ -464,8 +464,8 @@ __global__ __launch_bounds__(kRecMaxThreads, 4) void recurrence_bwd_kernel(RecPa
       const float g = up[i][k] + B[k];
       df[k] = g * ds[i][k];
       dc[k] = g * u[i][k];
-      sum[0][k] += df[k];
-      sum[1][k] += dc[k];
+      sum[0][k] += i < rows ? df[k] : 0.f;
+      sum[1][k] += i < rows ? dc[k] : 0.f;
       B[k] = f[i][k] * g;
     }
     dst.store(P::pack(df[0], df[1]), i, 0, i < rows);
