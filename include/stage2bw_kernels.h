@@ -114,7 +114,8 @@ int k2bw_attention_bwd(int dtype, int b, int s, int a, int dh, int mask_mode, co
  * pos[axis_of_pair_host[i]][token] * freq_host[i] radians (p' = p cos - q sin, q' = q cos + p sin), by minus that if inverse is not 0.
  * n_pairs: 1..dh/2, dh a multiple of 8 up to 128.  axis_of_pair_host: n_pairs bytes below n_axes (1..255), freq_host: n_pairs finite
  * numbers, both read before the call returns.  pos: [n_axes][b*s] (any int32), or NULL: the token's place in its sequence, on every axis.
- * V columns are never touched; rows of padding are turned like any others.  3h up to 2^30. */
+ * V columns are never touched; rows of padding are turned like any others.  3h up to 2^30; what does not fit into
+ * the 2^32 threads of a launch is refused (everything with b*s * ceil(a * n_pairs / 128) below 2^24 fits). */
 int k2bw_rotary(int dtype, int b, int s, int a, int dh, int n_pairs, int pairing, const uint8_t* axis_of_pair_host,
                 const double* freq_host, int n_axes, const int32_t* pos, int inverse, void* qkv, void* stream);
 
@@ -124,7 +125,8 @@ int k2bw_rotary(int dtype, int b, int s, int a, int dh, int n_pairs, int pairing
  * gates hold is not looked at.  state_in, state_out: fp32 [b, h] (may be NULL: zero, not wanted; may be the same array: s = 1 with both
  * is the step of a model that answers).  saved (may be NULL if there is no backward pass): k2bw_recurrence_saved(b, s, h) floats for
  * k2bw_recurrence_bwd.  workspace: k2bw_recurrence_workspace(b, s, h) floats of any contents, for either call; calls that may run at
- * the same time (streams, graphs) need one each.  h: multiple of 8 up to 2^20; b*s below 2^31. */
+ * the same time (streams, graphs) need one each.  h: multiple of 8 up to 2^20; b*s below 2^31; what does not fit into the 2^32 threads of a
+ * launch is refused (everything with b * ceil(s/64) * ceil(h/64) below 2^23 fits). */
 int64_t k2bw_recurrence_saved(int b, int s, int h);
 int64_t k2bw_recurrence_workspace(int b, int s, int h);
 int k2bw_recurrence_fwd(int dtype, int b, int s, int h, const int32_t* seqlens, const void* gates, const float* state_in,

@@ -110,6 +110,7 @@ __device__ __forceinline__ float gelu_grad_fast(float u) {
   return fmaf(u * 0.39894228040143268f, e, normal_cdf_fast(u));
 }
 
+constexpr int64_t kMaxThreads = 0xffffffff;   // of a launch, along a dimension
 inline int ceil_div(int64_t a, int64_t b) { return static_cast<int>((a + b - 1) / b); }
 
 }  // namespace k2bw

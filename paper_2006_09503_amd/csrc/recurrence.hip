@@ -496,25 +496,27 @@ __global__ __launch_bounds__(kRecMaxThreads, 4) void recurrence_bwd_kernel(RecPa
 
 template <typename T> constexpr int kRecRows = 8;   // rows of a sub
 
-struct RecShape { int waves, tiles, rows, groups; };
+struct RecShape { int waves, tiles, rows, groups; int64_t threads; };   // threads: of the launch
 template <typename T>
 RecShape rec_shape(int b, int s, int h) {
   constexpr int per_wave = kRecRows<T> * 64 / kRecLanes<T>;   // rows
   RecShape r;
   r.groups = ceil_div(h, 2 * kRecLanes<T>);
   r.waves = kRecWaves;
-  while (r.waves > 1 && per_wave * r.waves >= 2 * s) r.waves /= 2;
+  while (r.waves > 1 && (int64_t)per_wave * r.waves >= 2 * (int64_t)s) r.waves /= 2;
   r.rows = per_wave * r.waves;
   r.tiles = ceil_div(s, r.rows);
+  r.threads = (int64_t)r.tiles * b * r.groups * (64 * r.waves);
   return r;
 }
 constexpr int kRecMinTileRows = 64, kRecMinCols = 64;   // of a tile, where a sequence has more than one
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 bool rec_ok(const RecurrenceDesc& d) {
-  return d.b > 0 && d.s > 0 && d.h > 0 && d.h % 8 == 0 && (d.dtype == kF32 || d.dtype == kBF16) &&
-         (int64_t)d.b * d.s <= 0x7fffffff && d.h <= (1 << 20) && recurrence_workspace(d.b, d.s, d.h) > 0 &&
-         !(reinterpret_cast<uintptr_t>(d.seqlens) & 3);
+  if (d.b <= 0 || d.s <= 0 || d.h <= 0 || d.h % 8 != 0 || (d.dtype != kF32 && d.dtype != kBF16) || (int64_t)d.b * d.s > 0x7fffffff || d.h > (1 << 20))
+    return false;
+  const RecShape shape = d.dtype == kF32 ? rec_shape<float>(d.b, d.s, d.h) : rec_shape<bf16_t>(d.b, d.s, d.h);
+  return shape.threads <= kMaxThreads && recurrence_workspace(d.b, d.s, d.h) > 0 && !(reinterpret_cast<uintptr_t>(d.seqlens) & 3);
 }
 int64_t rec_max_tiles(int s) { return ((int64_t)s + kRecMinTileRows - 1) / kRecMinTileRows; }
 
@@ -535,7 +537,6 @@ hipError_t launch_rec(const RecurrenceDesc& d, RecParams p, float* ws, bool sums
   // 3 % (fp32 4096 x 4096 160 | 164).
   p.near = (int64_t)d.h * sizeof(T) % 128 != 0 || (int64_t)p.b * p.groups <= 16 ? 8 : 1;
   const int64_t grid = (int64_t)p.tiles * p.b * p.groups;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
   const int64_t bh = (int64_t)d.b * d.h;
   const int64_t tickets = rec_tickets(d.b, d.h);
   p.tickets = reinterpret_cast<uint32_t*>(ws);

@@ -141,7 +141,7 @@ hipError_t launch_rotary(RotaryParams p, hipStream_t s) {
   if (p.per_group > kRotMaxTokens) p.per_group = kRotMaxTokens;
   p.parts = items > kItems ? (items + kItems - 1) / kItems : 1;
   const int64_t groups = (p.tokens + p.per_group - 1) / p.per_group * p.parts;
-  if (groups > 0x7fffffff) return hipErrorInvalidValue;
+  if (groups * kRotThreads > kMaxThreads) return hipErrorInvalidValue;
   hipLaunchKernelGGL((rotary_kernel<T, V, HALF>), dim3((unsigned)groups), dim3(kRotThreads), 0, s, p);
   return hipGetLastError();
 }
