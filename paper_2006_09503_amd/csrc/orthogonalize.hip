@@ -14,9 +14,10 @@
 //
 // Two steps at a time where X is wide: A_1 = X_1 X_1' = P_1 A_0 P_1 needs no pass over X, and X_2 = (P_2 P_1) X_0 only one, so a pair costs
 //   gram A_0 (half of 2 m^2 n: symmetric), P_1, U = A_0 P_1, A_1 = U P_1, P_2, Q = P_2 P_1 (half of 2 m^3 each), X <- Q X (2 m^2 n)
-// against twice gram, P, X <- P X: 3 n + 5 m against 6 n + 2 m times m^2.  A_k's error grows with X's smallest singular values, a^2 times a
-// step: three steps lose too much in 16 bits (up to 1e-2), and nothing that shows in fp32, where the first of an odd number go three at a
-// time (3 n + 9 m against 9 n + 3 m).
+// against twice gram, P, X <- P X: 3 n + 5 m against 6 n + 2 m times m^2.  What A_0 is off by grows by a^2 on the smallest singular values; in front
+// the single steps behind divide it out again as those values grow, further back they do not, so in 16 bits only the first two go together: 1024 x
+// 4096 of rank 256 and 1 % noise, one step at a time | the first two together | two, one, two: 1.0e-3 | 1.0e-3 | 7.1e-3.  In fp32 the first of an odd
+// number go three at a time (3 n + 9 m against 9 n + 3 m).
 //
 // The means are sums of products of entries that the epilogues leave per tile and that whoever needs them adds up in one order, so
 // results do not depend on timing.  They are shifts that drop out of the polynomial: their own rounding does not matter.
@@ -1165,10 +1166,10 @@ struct OrthRun {
     // in the place of every pass it saves: 1024 x 1024 to 2048 x 2048 from n = 2 m on.
     const double passes = orth_tile<kGram>(l.mp, l.mp, l.np, d.count, split).cost + orth_tile<kUpdate>(l.mp, l.np, l.mp, d.count, split).cost;
     const bool several = passes > 3.0 * orth_tile<kMul>(l.mp, l.mp, l.mp, d.count, split).cost + 2.0;
-    // 16 bits: pairs from both ends, an odd step between them.  fp32: an odd number begins with three.
+    // 16 bits: a pair in front of two single steps at least.  fp32: pairs, an odd number begins with three.
     for (int i = 0; i < d.steps;) {
-      const bool odd = d.steps % 2 && i == (split ? 0 : d.steps / 4 * 2);
-      const int n = !several || i + 1 == d.steps ? 1 : !odd ? 2 : split ? 3 : 1;
+      const bool odd = d.steps % 2 && i == 0;
+      const int n = !several || i + 1 == d.steps ? 1 : !split ? (i == 0 && d.steps >= 4 ? 2 : 1) : odd ? 3 : 2;
       const hipError_t e = n == 3 ? three(i) : n == 2 ? two(i) : one(i);
       if (e != hipSuccess) return e;
       i += n;
