@@ -174,7 +174,8 @@ int k2bw_momentum(int64_t n, const float* w_cur, float* w_next, void* w_next_bf1
  * of out are near 1.  coef_host: a, b, c of each of the `steps` (1..64), read before the call returns; NULL: 3.4445, -4.7750, 2.0315
  * every time.  (Other coefficients have to keep singular values below 3: larger ones end outside fp16.)  The products take 16-bit
  * operands in bf16 (five default steps are off by 2e-4 to 2e-3 of the result, 2-norm, a bf16 result's own rounding being 1.7e-3; by up to 1e-2
- * where a few rows or directions are more than a hundred times the others) and fp32 accuracy in fp32.  rows: any number; cols, ld and
+ * where a few rows or directions are more than a hundred times the others) and fp32 accuracy in fp32
+ * (what the iteration in 32-bit arithmetic is off by).  rows: any number; cols, ld and
  * stride: multiples of 8; rows and cols up to 4194240, their product, both padded to multiples of 64, below 2^30 (fp32: up to 2^29), count up
  * to 65535.  A matrix with an infinity or a NaN comes out as NaN, the others of its batch do not notice.  workspace:
  * k2bw_orthogonalize_workspace floats of any contents; calls that may run at the same time need one each. */

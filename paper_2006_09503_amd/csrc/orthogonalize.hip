@@ -6,18 +6,21 @@
 // two fp16 numbers (hi + lo, 22 bits); the matrix cores multiply the fp16 parts, everything linear takes both:
 //   L R = mean_L mean_R I + mean_R L' + mean_L R' + L' R',    X <- mean_P X + P' X.
 // What the matrices are on average never passes through 11 bits that way, and X is only rounded where it is multiplied by a P' of mean
-// zero.  Off the 64-bit result by 2e-4 to 1.6e-3 (2-norm; the most for matrices of a small rank and little else), less than a bf16
-// result's own rounding; with fp16 numbers for all of A, P and X 4e-4 to 2e-2, with bf16 1e-2 to 1.7e-1.  fp32 results take three
-// products, hi hi + hi lo + lo hi: 1e-6, at three times the matrix time, where the fp32 matrix instructions take sixteen.  A K tile holds both
+// zero.  Off the 64-bit result after five default steps (2-norm): 2e-4 to 2e-3 (the most for small ranks and little else), a bf16 result's own
+// rounding being 1.7e-3, and up to 1e-2 where a few rows or directions are more than a hundred times the others; with fp16 numbers for all of A, P
+// and X 4e-4 to 2e-2, with bf16 1e-2 to 1.7e-1.  fp32 results take three products, hi hi + hi lo + lo hi: 3e-7 to 2e-4, 0.04 to 1 times what the
+// iteration in 32-bit arithmetic is off by on this card (2.3 times, 1.1e-6, beside one row that is 300 times the others), at three times the matrix
+// time, where the fp32 matrix instructions take sixteen.  A K tile holds both
 // planes of either operand and gives all three (gemm_lds.hpp's PLANES): operands arrive at about 36 bytes a cycle and CU in every shape, and the
 // products one after the other, of planes fetched three times, take 1.05 (2560 x 10240) to 1.24 (943 x 3768) of the time.
 //
-// Two steps at a time where X is wide: A_1 = X_1 X_1' = P_1 A_0 P_1 needs no pass over X, and X_2 = (P_2 P_1) X_0 only one, so a pair costs
+// The first two steps together where X is wide: A_1 = X_1 X_1' = P_1 A_0 P_1 needs no pass over X, and X_2 = (P_2 P_1) X_0 only one, so they cost
 //   gram A_0 (half of 2 m^2 n: symmetric), P_1, U = A_0 P_1, A_1 = U P_1, P_2, Q = P_2 P_1 (half of 2 m^3 each), X <- Q X (2 m^2 n)
 // against twice gram, P, X <- P X: 3 n + 5 m against 6 n + 2 m times m^2.  What A_0 is off by grows by a^2 on the smallest singular values; in front
-// the single steps behind divide it out again as those values grow, further back they do not, so in 16 bits only the first two go together: 1024 x
-// 4096 of rank 256 and 1 % noise, one step at a time | the first two together | two, one, two: 1.0e-3 | 1.0e-3 | 7.1e-3.  In fp32 the first of an odd
-// number go three at a time (3 n + 9 m against 9 n + 3 m).
+// the single steps behind divide it out again as those values grow, further back they do not.  1024 x 4096 | 1536 x 4608 of rank m/4 and 1 % noise, with
+// two, one, two together: bf16 results off by 7.1e-3 | 7.3e-3, so 1.9e-3 | 1.9e-3 (1.7e-3 of it rounding; 1.0e-3 is what single steps are off by before
+// it).  fp32, three and two together 7.0e-6 | 1.5e-5, so 4.5e-6 | 4.5e-6, the 32-bit iteration 8.7e-6 | 8.3e-6.  Three in front, fp32: up to 6 times that
+// beside one row that is 300 times the others.
 //
 // The means are sums of products of entries that the epilogues leave per tile and that whoever needs them adds up in one order, so
 // results do not depend on timing.  They are shifts that drop out of the polynomial: their own rounding does not matter.
@@ -32,8 +35,8 @@ namespace {
 
 constexpr int kPad = 64;
 // Powers of two that the fp16 numbers are kept at.  X has entries of at most about 1.2 (its singular values' bound) and of 1 / sqrt(m n) to
-// begin with; A and A P of at most 1.5; P and P P of at most a^2 = 12, three of them a^3 = 41.
-constexpr float kScaleX = 4096.f, kScaleA = 4096.f, kScaleP = 1024.f, kScaleQ = 128.f;
+// begin with; A and A P of at most 1.5; P and P P of at most a^2 = 12.
+constexpr float kScaleX = 4096.f, kScaleA = 4096.f, kScaleP = 1024.f;
 
 enum Product : int { kGram = 0, kMul = 1, kUpdate = 2, kLast = 3 };   // X X'; L R of two m x m matrices; X <- P X; the same to where X leaves for
 
@@ -909,11 +912,11 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 
 struct OrthLayout {
   int m, n, mp, np;
   int64_t x_plane, m_plane;                                  // bytes
-  int64_t x[2], mat[4], x_sums, m_sums[2], squares, means, size;
+  int64_t x[2], mat[3], x_sums, m_sums[2], squares, means, size;
   int n_squares;
 };
 constexpr int kMaxSquares = 256;
-OrthLayout orth_layout(int dtype, int rows, int cols) {
+OrthLayout orth_layout(int rows, int cols) {
   OrthLayout l;
   l.m = rows < cols ? rows : cols;
   l.n = rows < cols ? cols : rows;
@@ -924,10 +927,10 @@ OrthLayout orth_layout(int dtype, int rows, int cols) {
   int64_t at = 0;
   auto take = [&](int64_t bytes) { const int64_t was = at; at += up(bytes, 256); return was; };
   for (int64_t& x : l.x) x = take(2 * l.x_plane);
-  for (int64_t& x : l.mat) x = &x == l.mat + 3 && dtype != kF32 ? -1 : take(2 * l.m_plane);   // (three steps at once: fp32)
+  for (int64_t& x : l.mat) x = take(2 * l.m_plane);
   l.x_sums = take(tm * tn * 4);
   for (int64_t& x : l.m_sums) x = take(tm * tm * 4);
-  l.squares = take(kMaxSquares * 8); l.means = take(4 * 4);
+  l.squares = take(kMaxSquares * 8); l.means = take(3 * 4);
   l.size = at;
   const int64_t chunks = ((int64_t)rows * (cols / 8) + 2047) / 2048;   // 8 vectors a thread
   l.n_squares = (int)(chunks < 1 ? 1 : chunks > kMaxSquares ? kMaxSquares : chunks);
@@ -1102,9 +1105,8 @@ struct OrthRun {
     return launch_product<kGram>(p, {}, d.count, &m_sums, stream);
   }
   // mat[out] = mat[left] mat[right] (coef: a + b L + c L^2 instead); the sums that the next product, of out with mat[partner], takes its mean
-  // from (partner = out: with itself).  mean: whether the sums there are are this product's; without, its mean stays where it is, in the
-  // rest, which in two fp16 numbers (fp32) loses nothing.
-  hipError_t mul(int out, int left, int right, float sl, float sr, float so, int partner, const float* coef, bool mean = true) {
+  // from (partner = out: with itself).
+  hipError_t mul(int out, int left, int right, float sl, float sr, float so, int partner, const float* coef) {
     OrthProduct p = base;
     p.A = at(l.mat[left]); p.B = at(l.mat[right]);
     p.M = p.N = p.K = p.lda = p.ldb = p.ldo = l.mp;
@@ -1115,7 +1117,7 @@ struct OrthRun {
     p.mean_left = left; p.mean_right = right; p.mean_out = out;
     p.scale_left = sl; p.scale_right = sr; p.scale_out = so;
     if (coef) { p.poly = 1; p.a = coef[0]; p.b = coef[1]; p.c = coef[2]; }
-    p.sums_in = sums(l.m_sums[at_sums]); p.n_sums = mean ? m_sums : 0;
+    p.sums_in = sums(l.m_sums[at_sums]); p.n_sums = m_sums;
     p.sums_out = sums(l.m_sums[at_sums ^= 1]);
     return launch_product<kMul>(p, {}, d.count, &m_sums, stream);
   }
@@ -1139,42 +1141,24 @@ struct OrthRun {
     if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 1, coef(step));
     return e == hipSuccess ? update(1, kScaleP, step + 1 == d.steps) : e;
   }
-  hipError_t two(int step) {
+  hipError_t two() {   // the first ones
     hipError_t e = gram();                                                                  // A_0
-    if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 0, coef(step));        // P_1
+    if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 0, coef(0));           // P_1
     if (e == hipSuccess) e = mul(2, 0, 1, kScaleA, kScaleP, kScaleA, 1, nullptr);           // U = A_0 P_1
     if (e == hipSuccess) e = mul(0, 2, 1, kScaleA, kScaleP, kScaleA, 0, nullptr);           // A_1 = U P_1
-    if (e == hipSuccess) e = mul(2, 0, 0, kScaleA, kScaleA, kScaleP, 1, coef(step + 1));    // P_2
+    if (e == hipSuccess) e = mul(2, 0, 0, kScaleA, kScaleA, kScaleP, 1, coef(1));           // P_2
     if (e == hipSuccess) e = mul(0, 2, 1, kScaleP, kScaleP, kScaleP, 0, nullptr);           // Q = P_2 P_1
-    return e == hipSuccess ? update(0, kScaleP, step + 2 == d.steps) : e;
-  }
-  hipError_t three(int step) {
-    hipError_t e = gram();                                                                  // A_0
-    if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 0, coef(step));        // P_1
-    if (e == hipSuccess) e = mul(2, 0, 1, kScaleA, kScaleP, kScaleA, 1, nullptr);           // A_0 P_1
-    if (e == hipSuccess) e = mul(0, 2, 1, kScaleA, kScaleP, kScaleA, 0, nullptr);           // A_1
-    if (e == hipSuccess) e = mul(2, 0, 0, kScaleA, kScaleA, kScaleP, 1, coef(step + 1));    // P_2
-    if (e == hipSuccess) e = mul(3, 2, 1, kScaleP, kScaleP, kScaleP, 3, nullptr);           // Q = P_2 P_1
-    if (e == hipSuccess) e = mul(1, 0, 2, kScaleA, kScaleP, kScaleA, 2, nullptr, false);    // A_1 P_2 (the sums in hand are Q's)
-    if (e == hipSuccess) e = mul(0, 1, 2, kScaleA, kScaleP, kScaleA, 0, nullptr);           // A_2
-    if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 3, coef(step + 2));    // P_3
-    if (e == hipSuccess) e = mul(0, 1, 3, kScaleP, kScaleP, kScaleQ, 0, nullptr);           // P_3 Q
-    return e == hipSuccess ? update(0, kScaleQ, step + 3 == d.steps) : e;
+    return e == hipSuccess ? update(0, kScaleP, false) : e;
   }
   hipError_t all() {
-    // Several steps on one pass over X, where a pass costs more than the three m x m products, and the launch (about 2 us), that a pair has
-    // in the place of every pass it saves: 1024 x 1024 to 2048 x 2048 from n = 2 m on.
+    // The first two steps on one pass over X, where a pass costs more than the three m x m products, and the launch (about 2 us), that the pair has
+    // in its place: 1024 x 1024 to 2048 x 2048 from n = 2 m on.
     const double passes = orth_tile<kGram>(l.mp, l.mp, l.np, d.count, split).cost + orth_tile<kUpdate>(l.mp, l.np, l.mp, d.count, split).cost;
-    const bool several = passes > 3.0 * orth_tile<kMul>(l.mp, l.mp, l.mp, d.count, split).cost + 2.0;
-    // 16 bits: a pair in front of two single steps at least.  fp32: pairs, an odd number begins with three.
-    for (int i = 0; i < d.steps;) {
-      const bool odd = d.steps % 2 && i == 0;
-      const int n = !several || i + 1 == d.steps ? 1 : !split ? (i == 0 && d.steps >= 4 ? 2 : 1) : odd ? 3 : 2;
-      const hipError_t e = n == 3 ? three(i) : n == 2 ? two(i) : one(i);
-      if (e != hipSuccess) return e;
-      i += n;
-    }
-    return hipSuccess;
+    const bool cheaper = passes > 3.0 * orth_tile<kMul>(l.mp, l.mp, l.mp, d.count, split).cost + 2.0;
+    const bool pair = cheaper && d.steps >= 4;
+    hipError_t e = pair ? two() : one(0);
+    for (int i = pair ? 2 : 1; i < d.steps && e == hipSuccess; ++i) e = one(i);
+    return e;
   }
 };
 
@@ -1196,7 +1180,7 @@ hipError_t launch_small_orth(const OrthDesc& d, const OrthEnds& e, const OrthSma
 // 275, 32 x 1024 223 | 889, 64 x 512 286 | 626, 128 x 128 265 | 622.
 template <typename T, bool MUON>
 hipError_t orth_run(const OrthDesc& d, OrthEnds e, float* workspace, hipStream_t s) {
-  const OrthLayout l = orth_layout(d.dtype, d.rows, d.cols);
+  const OrthLayout l = orth_layout(d.rows, d.cols);
   char* ws = reinterpret_cast<char*>(workspace);
   e.rows = d.rows; e.cols = d.cols; e.tall = d.rows > d.cols;
   e.X = reinterpret_cast<bf16_t*>(ws + l.x[0]); e.plane = l.x_plane / 2; e.matrix = l.size; e.ldx = l.np;
@@ -1238,7 +1222,7 @@ int64_t orthogonalize_workspace(const OrthDesc& d) {   // floats
   OrthDesc one = d;
   one.steps = 1;
   if (!orth_ok(one)) return 0;
-  return orth_layout(d.dtype, d.rows, d.cols).size / 4 * d.count;
+  return orth_layout(d.rows, d.cols).size / 4 * d.count;
 }
 
 hipError_t orthogonalize(const OrthDesc& d, const void* in, int ld_in, int64_t in_stride, void* out, int ld_out, int64_t out_stride,

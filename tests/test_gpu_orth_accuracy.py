@@ -92,7 +92,7 @@ SIZES = [(1024, 4096), (1536, 4608), (4608, 1536), (700, 4200)]
 
 @pytest.mark.parametrize("size", SIZES, ids=str)
 @pytest.mark.parametrize("part, noise", [(4, 0.01), (16, 0.01), (6, 0.0), (2, 0.0), (16, 1.0)], ids=str)
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_small_ranks(dtype, part, noise, size):
     g = torch.Generator(device="cuda").manual_seed(sum(size) + part)
     u = low_rank(g, *size, min(size) // part, noise) * 1e-3
@@ -100,14 +100,14 @@ def test_small_ranks(dtype, part, noise, size):
 
 
 @pytest.mark.parametrize("steps", [2, 3, 4, 6, 7])
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_small_ranks_by_numbers_of_steps(dtype, steps):
     g = torch.Generator(device="cuda").manual_seed(steps)
     u = low_rank(g, 700, 4200, 175, 0.01) * 1e-3
     check(dtype, u.bfloat16() if dtype == BF16 else u, steps)
 
 
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_of_unequal_size(dtype):
     g = torch.Generator(device="cuda").manual_seed(1)
     u = torch.randn((1024, 4096), generator=g, device="cuda") * torch.logspace(-6, -3, 1024, device="cuda")[:, None]
