@@ -172,7 +172,8 @@ int k2bw_momentum(int64_t n, const float* w_cur, float* w_next, void* w_next_bf1
  * rows ld elements apart; out may be in): X = U / |U| (Frobenius norm; zeros stay zeros), then per step
  * X <- a X + (b A + c A^2) X with A = X X' (X' X where there are more rows than columns: the same map), after which the singular values
  * of out are near 1.  coef_host: a, b, c of each of the `steps` (1..64), read before the call returns; NULL: 3.4445, -4.7750, 2.0315
- * every time.  (Other coefficients have to keep singular values below 3: larger ones end outside fp16.)  The products take 16-bit
+ * every time.  (Other coefficients have to keep X's singular values below 3 and a + b l + c l^2 within 30 for A's eigenvalues l: what is larger
+ * ends outside fp16.)  The products take 16-bit
  * operands in bf16 (five default steps are off by 2e-4 to 2e-3 of the result, 2-norm, a bf16 result's own rounding being 1.7e-3; by up to 1e-2
  * where a few rows or directions are more than a hundred times the others) and fp32 accuracy in fp32
  * (what the iteration in 32-bit arithmetic is off by).  rows: any number; cols, ld and

@@ -947,6 +947,27 @@ bool orth_ok(const OrthDesc& d) {
 }
 
 constexpr float kQuintic[3] = {3.4445f, -4.7750f, 2.0315f};
+const float* orth_coef(const OrthDesc& d, int step) { return d.coef ? d.coef + 3 * step : kQuintic; }
+
+// Whether the first two steps may be taken together: the polynomials a + b l + c l^2 of both stay within 3.5 (the default's a is 3.4445) on the
+// eigenvalues l that A can have there, [0, 1] and what becomes of them.  What A_0 is off by grows with the first one squared, and fp16 holds their
+// product up to 64.
+bool orth_mild(const OrthDesc& d) {
+  double s = 1.0;   // X's largest singular value
+  for (int i = 0; i < 2; ++i) {
+    const float* k = orth_coef(d, i);
+    const double a = k[0], b = k[1], c = k[2], top = s * s, turn = -b / (2.0 * c), root = std::sqrt(std::max(0.0, 9.0 * b * b - 20.0 * a * c));
+    auto P = [&](double l) { return std::fabs(a + b * l + c * l * l); };
+    double most = std::max(P(0.0), P(top)), next = s * P(top);
+    if (turn > 0.0 && turn < top) most = std::max(most, P(turn));
+    if (!(most <= 3.5)) return false;
+    // s P(s^2) is largest at the end or where a + 3 b l + 5 c l^2 = 0 (c = 0: a + 3 b l)
+    for (const double l : {(-3.0 * b + root) / (10.0 * c), (-3.0 * b - root) / (10.0 * c), -a / (3.0 * b)})
+      if (l > 0.0 && l < top) next = std::max(next, std::sqrt(l) * P(l));
+    s = next;
+  }
+  return true;
+}
 
 template <typename K>
 hipError_t more_lds(K kernel, size_t lds, bool (&configured)[64]) {
@@ -1135,7 +1156,7 @@ struct OrthRun {
     if (last) return launch_product<kLast>(p, ends, d.count, &x_sums, stream);
     return launch_product<kUpdate>(p, {}, d.count, &x_sums, stream);
   }
-  const float* coef(int step) const { return d.coef ? d.coef + 3 * step : kQuintic; }
+  const float* coef(int step) const { return orth_coef(d, step); }
   hipError_t one(int step) {
     hipError_t e = gram();
     if (e == hipSuccess) e = mul(1, 0, 0, kScaleA, kScaleA, kScaleP, 1, coef(step));
@@ -1155,7 +1176,7 @@ struct OrthRun {
     // in its place: 1024 x 1024 to 2048 x 2048 from n = 2 m on.
     const double passes = orth_tile<kGram>(l.mp, l.mp, l.np, d.count, split).cost + orth_tile<kUpdate>(l.mp, l.np, l.mp, d.count, split).cost;
     const bool cheaper = passes > 3.0 * orth_tile<kMul>(l.mp, l.mp, l.mp, d.count, split).cost + 2.0;
-    const bool pair = cheaper && d.steps >= 4;
+    const bool pair = cheaper && d.steps >= 4 && orth_mild(d);
     hipError_t e = pair ? two() : one(0);
     for (int i = pair ? 2 : 1; i < d.steps && e == hipSuccess; ++i) e = one(i);
     return e;

@@ -112,3 +112,19 @@ def test_rows_of_unequal_size(dtype):
     g = torch.Generator(device="cuda").manual_seed(1)
     u = torch.randn((1024, 4096), generator=g, device="cuda") * torch.logspace(-6, -3, 1024, device="cuda")[:, None]
     check(dtype, u.bfloat16() if dtype == BF16 else u)
+
+
+# 2.9 T5(s), 2.9 T5(s / 2.9), T5 the Chebyshev polynomial 16 s^5 - 20 s^3 + 5 s: within 2.9 on [0, 1] and on what that gives, and 72.5 times what is
+# small; then halves.
+STEEP = (14.5, -58.0, 46.4, 5.0, -20.0 / 2.9 ** 2, 16.0 / 2.9 ** 4, 0.5, 0.0, 0.0, 0.5, 0.0, 0.0, 1.5, -0.5, 0.0)
+
+
+@pytest.mark.parametrize("rows, cols", [(704, 4200), (4200, 704)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_coefficients_whose_product_leaves_fp16(dtype, rows, cols):
+    """Few rows are not zero, so what a product of two steps' polynomials has on the diagonal reaches from its mean, 69, to under 0."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    u = torch.zeros((704, 4200), device="cuda")
+    u[::16] = torch.randn((44, 4200), generator=g, device="cuda")
+    u = (u if rows < cols else u.T).contiguous()
+    check(dtype, u.bfloat16() if dtype == BF16 else u, 5, STEEP)
