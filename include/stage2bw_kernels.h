@@ -169,7 +169,7 @@ int k2bw_momentum(int64_t n, const float* w_cur, float* w_next, void* w_next_bf1
                   const float* G, float lr, float beta, int m_micro, void* stream);
 
 /* Orthogonalised updates.  in -> out for `count` matrices [rows, cols] of element type dtype (matrix i at base + i * stride elements,
- * rows ld elements apart; out may be in): X = U / |U| (Frobenius norm; zeros stay zeros), then per step
+ * rows ld elements apart; matrices of out share no element; out may be in, with the same ld and stride where there are several): X = U / |U| (Frobenius norm; zeros stay zeros), then per step
  * X <- a X + (b A + c A^2) X with A = X X' (X' X where there are more rows than columns: the same map), after which the singular values
  * of out are near 1.  coef_host: a, b, c of each of the `steps` (1..64), read before the call returns; NULL: 3.4445, -4.7750, 2.0315
  * every time.  (Other coefficients have to keep X's singular values below 3 and a + b l + c l^2 within 30 for A's eigenvalues l: what is larger
@@ -188,7 +188,7 @@ int k2bw_orthogonalize(int dtype, int count, int rows, int cols, const void* in,
  * m <- beta m + (1-beta) g, u = nesterov ? beta m + (1-beta) g : m, w_next = w_cur (1 - lr weight_decay) - lr scale orthogonal(u)
  * (scale 0.2 sqrt(max(rows, cols)) gives the update an Adam step's usual size), and, if w_next_bf16 is not NULL, its bf16 rounding.
  * All arrays fp32 with one ld and stride, so the matrices of a stage's layers, or the Q, K and V columns of one (ld = 3h, stride = h),
- * are one call on the flat parameter vectors; what lies between the matrices stays as it is.  w_next may be w_cur.  dtype: the
+ * are one call on the flat parameter vectors; matrices share no element, and what lies between them stays as it is.  w_next may be w_cur.  dtype: the
  * products' operands, as above. */
 int k2bw_muon(int dtype, int count, int rows, int cols, int ld, int64_t stride, const float* w_cur, float* w_next, void* w_next_bf16,
               float* m, const float* G, float lr, float beta, float weight_decay, float scale, int nesterov, int m_micro, int steps,

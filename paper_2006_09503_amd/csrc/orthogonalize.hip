@@ -1237,6 +1237,15 @@ bool matrix_ok(const OrthDesc& d, int ld, int64_t stride) {
   return ld >= d.cols && ld % 8 == 0 && stride % 8 == 0 && (d.count == 1 || stride > 0) && ld <= (1 << 30);
 }
 
+// Whether no two of the matrices share an element: the distance of two is not within `cols` of a number of rows that both have.
+bool apart(const OrthDesc& d, int ld, int64_t stride) {
+  for (int64_t i = 1, at = stride; i < d.count && at < (int64_t)(d.rows - 1) * ld + d.cols; ++i, at += stride) {
+    const int64_t row = at / ld, col = at % ld;
+    if (col < d.cols || (ld - col < d.cols && row + 1 < d.rows)) return false;
+  }
+  return true;
+}
+
 }  // namespace
 
 int64_t orthogonalize_workspace(const OrthDesc& d) {   // floats
@@ -1249,7 +1258,8 @@ int64_t orthogonalize_workspace(const OrthDesc& d) {   // floats
 hipError_t orthogonalize(const OrthDesc& d, const void* in, int ld_in, int64_t in_stride, void* out, int ld_out, int64_t out_stride,
                          float* workspace, hipStream_t stream) {
   if (!orth_ok(d) || !matrix_ok(d, ld_in, in_stride) || !matrix_ok(d, ld_out, out_stride) || !in || !out || !workspace || !aligned16(in) ||
-      !aligned16(out) || !aligned16(workspace))
+      !aligned16(out) || !aligned16(workspace) || !apart(d, ld_out, out_stride) ||
+      (in == out && d.count > 1 && (ld_in != ld_out || in_stride != out_stride)))
     return hipErrorInvalidValue;
   OrthEnds e{};
   e.kind = d.dtype == kF32 ? kEndF32 : kEndBf16;
@@ -1259,7 +1269,7 @@ hipError_t orthogonalize(const OrthDesc& d, const void* in, int ld_in, int64_t i
 
 hipError_t muon_step(const OrthDesc& d, const MuonDesc& u, float* workspace, hipStream_t stream) {
   if (!orth_ok(d) || !matrix_ok(d, u.ld, u.stride) || !u.w_cur || !u.w_next || !u.m || !u.G || !workspace || !aligned16(u.w_cur) ||
-      !aligned16(u.w_next) || !aligned16(u.m) || !aligned16(u.G) || !aligned16(u.w_next_lp) || !aligned16(workspace))
+      !aligned16(u.w_next) || !aligned16(u.m) || !aligned16(u.G) || !aligned16(u.w_next_lp) || !aligned16(workspace) || !apart(d, u.ld, u.stride))
     return hipErrorInvalidValue;
   OrthEnds e{};
   e.kind = kEndMuon;
