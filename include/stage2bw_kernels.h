@@ -112,8 +112,8 @@ int k2bw_attention_bwd(int dtype, int b, int s, int a, int dh, int mask_mode, co
  * inverse = 1 on dqkv it is the backward pass.  The first 2 * n_pairs elements of every head are pairs (p, q): elements i and
  * i + n_pairs (pairing 0) or 2i and 2i + 1 (pairing 1); the rest of the head stays as it is.  Pair i turns by
  * pos[axis_of_pair_host[i]][token] * freq_host[i] radians (p' = p cos - q sin, q' = q cos + p sin), by minus that if inverse is not 0.
- * n_pairs: 1..dh/2, dh a multiple of 8 up to 128.  axis_of_pair_host: n_pairs bytes below n_axes (1..255), freq_host: n_pairs finite
- * numbers, both read before the call returns.  pos: [n_axes][b*s] (any int32), or NULL: the token's place in its sequence, on every axis.
+ * n_pairs: 1..dh/2, dh a multiple of 8 up to 128.  axis_of_pair_host: n_pairs bytes below n_axes (1..255), freq_host: n_pairs
+ * numbers up to 2^900 in size (an angle is off by 2^-52 of itself), both read before the call returns.  pos: [n_axes][b*s] (any int32), or NULL: the token's place in its sequence, on every axis.
  * V columns are never touched; rows of padding are turned like any others.  3h up to 2^30; what does not fit into
  * the 2^32 threads of a launch is refused (everything with b*s * ceil(a * n_pairs / 128) below 2^24 fits). */
 int k2bw_rotary(int dtype, int b, int s, int a, int dh, int n_pairs, int pairing, const uint8_t* axis_of_pair_host,

@@ -176,7 +176,7 @@ hipError_t rotary(const RotaryDesc& d, void* x, hipStream_t stream) {
   p.x = x; p.pos = d.pos; p.tokens = (int64_t)d.b * d.s; p.s = d.s; p.row = 3 * d.a * d.dh; p.dh = d.dh; p.n = d.n_pairs;
   p.heads2 = 2 * d.a; p.inverse = d.inverse ? 1 : 0;
   for (int i = 0; i < d.n_pairs; ++i) {
-    if (d.axis_of_pair[i] >= d.n_axes || !std::isfinite(d.freq[i])) return hipErrorInvalidValue;
+    if (d.axis_of_pair[i] >= d.n_axes || !(std::fabs(d.freq[i]) <= 0x1p900)) return hipErrorInvalidValue;   // (positions times it: finite)
     p.axis[i] = d.axis_of_pair[i];
     p.turns[i] = d.freq[i] / 6.283185307179586476925286766559;
   }

@@ -35,6 +35,12 @@ def test_rotary_refuses_more_than_a_launch_holds(case):
     assert B.lib().k2bw_rotary(dtype, b, s, a, dh, n, pairing, axis, freq, 1, None, 0, P, None) == B.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("freq", [float("nan"), float("inf"), 1e300, -1.7e308])
+def test_rotary_refuses_frequencies_whose_angles_are_not_finite(freq):
+    axis, f = (ctypes.c_uint8 * 4)(), (ctypes.c_double * 4)(1.0, 1.0, 1.0, freq)
+    assert B.lib().k2bw_rotary(0, 1, 1, 1, 8, 4, 0, axis, f, 1, None, 0, P, None) == B.ERR_INVALID_ARG
+
+
 def orthogonalize(count, rows, cols, ld_in, stride_in, ld_out, stride_out, out=2 * P):
     return B.lib().k2bw_orthogonalize(1, count, rows, cols, P, ld_in, stride_in, out, ld_out, stride_out, 5, None, 4 * P, None)
 
