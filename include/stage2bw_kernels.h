@@ -1,6 +1,8 @@
 /*
  * stage2bw_kernels.h -- C ABI of the single kernels the 2BW stage is made of, for parity tests
- * and stand-alone roofline measurements.  Every pointer is a DEVICE pointer owned by the caller
+ * and stand-alone roofline measurements, and of operators that a program uses beside them (rotary
+ * positions, the gated linear recurrence, orthogonalised updates: stage_t has no setting for
+ * these).  Every pointer is a DEVICE pointer owned by the caller
  * unless its name ends in _host; `stream` is a hipStream_t (NULL = null stream).  Calls only
  * enqueue.  Return value: 0, or a negative STAGE_ERR_* code from stage2bw.h (INVALID_ARG when a
  * shape or alignment the kernel assumes does not hold; nothing is launched then).
@@ -187,8 +189,9 @@ int k2bw_orthogonalize(int dtype, int count, int rows, int cols, const void* in,
 /* The optimizer step made of it, for matrices beside k2bw_adam for everything else, from the coalesced sum G: g = G/m_micro,
  * m <- beta m + (1-beta) g, u = nesterov ? beta m + (1-beta) g : m, w_next = w_cur (1 - lr weight_decay) - lr scale orthogonal(u)
  * (scale 0.2 sqrt(max(rows, cols)) gives the update an Adam step's usual size), and, if w_next_bf16 is not NULL, its bf16 rounding.
- * All arrays fp32 with one ld and stride, so the matrices of a stage's layers, or the Q, K and V columns of one (ld = 3h, stride = h),
- * are one call on the flat parameter vectors; matrices share no element, and what lies between them stays as it is.  w_next may be w_cur.  dtype: the
+ * All arrays fp32 with one ld and stride, so a program whose parameters lie flat, layer after layer, updates one matrix of all layers, or the
+ * Q, K and V columns of one (ld = 3h, stride = h), in one call (a stage_t keeps its vectors to itself and updates them by Adam or momentum);
+ * matrices share no element, and what lies between them stays as it is.  w_next may be w_cur.  dtype: the
  * products' operands, as above. */
 int k2bw_muon(int dtype, int count, int rows, int cols, int ld, int64_t stride, const float* w_cur, float* w_next, void* w_next_bf16,
               float* m, const float* G, float lr, float beta, float weight_decay, float scale, int nesterov, int m_micro, int steps,

@@ -5,7 +5,7 @@
 //   dC_t = u_t g_t,  dF_t = g_t (h_(t-1) - C_t) f_t u_t,  dR_t = dO_t h_t sigmoid(R_t) (1 + R_t sigmoid(-R_t)).
 // (u is computed from F by itself: 1 - f has no digits left where a memory is long.)
 //
-// Both directions are scans with maps x -> A x + H, which compose: (A1, H1) then (A2, H2) is (A1 A2, A2 H1 + H2).  A workgroup owns a
+// Both directions are scans with maps x -> A x + H, in a single pass with look back (Merrill and Garland, 2016); the maps compose: (A1, H1) then (A2, H2) is (A1 A2, A2 H1 + H2).  A workgroup owns a
 // tile of rows x 128 channels (bf16; 64 in fp32: 256 bytes of a row).  A sub -- a wave, or half of one in fp32 -- holds 8 consecutive rows of
 // it, two channels per lane, in registers, and reduces them to their map; the subs' maps meet in LDS, the tile's own map is published, the
 // state that enters the tile comes from the tiles in front of it (behind it, backward), and the rows are gone through once more, from
@@ -20,9 +20,10 @@
 // waits only for workgroups of its chain that have started, and of those that wait the one with the lowest ticket waits for nobody, so
 // every wait ends.
 //
-// Bound by the vector unit and by the latencies of a workgroup's life (ticket, loads, maps, stores) about alike; HBM's part at the rate of
-// the same streams with nothing computed is 24 of 33 us forward, 45 of 58 backward (2048 x 8192 bf16, without the launches that clear the
-// words and finish the sums).  Two workgroups of eight waves on a CU: forward 94 registers, backward 128, which is all there are for
+// fp32: bound by its streams (32768 x 1000: forward 139 us, backward 207, where the same rows loaded and stored with nothing computed take 124 and 215;
+// rows of 4000 bytes share lines).  bf16: 34 and 60 us for 2048 x 8192, where the streams alone take 21 and 37: vector instructions are at work half of
+// the time and waves wait half of theirs (profiles/operators_counters.txt), the latencies of a workgroup's life (ticket, loads, maps, stores).  The
+// launches that clear the words and finish the sums come on top.  Two workgroups of eight waves on a CU: forward 94 registers, backward 128, which is all there are for
 // two.  Forced to more, the spills cost more than the waves bring (forward at 80 registers 55 us, backward at 96 144); 16 waves: even
 // forward, 8 % behind backward; 4 rows per sub: 10 % behind.
 //
@@ -72,7 +73,7 @@ template <> struct Pair<bf16_t> {
 // is 2^-124 and the other 1 (a reciprocal further down would be flushed to zero); a NaN stays one.  The reciprocal instruction's own error
 // goes the same way at every token, and a memory of hundreds adds it up.  fp32: near 1 the one is 1 minus the other, off by the rounding of
 // that alone (32768 tokens: results off by 2.2e-7 instead of 8.7e-7).  bf16, whose states and their gradients leave in fp32: a Newton step, an
-// instruction less (the carried gradient off by 3.6e-7 instead of 1.2e-6; backward of 2048 x 8192 58 -> 61 us, 64 the other way).
+// instruction less (the carried gradient off by 3.6e-7 instead of 1.2e-6; backward of 2048 x 8192 59 us without it, 60 with, 63 the other way).
 template <typename T>
 __device__ __forceinline__ void sigmoids(float x, float& pos, float& neg) {
   const float z = __builtin_elementwise_minimum(Pair<T>::exp_neg(x), 0x1p124f);

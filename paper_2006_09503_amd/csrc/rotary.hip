@@ -4,11 +4,13 @@
 // t = pos[x(i)][token] * freq(i):  p' = p cos t - q sin t,  q' = q cos t + p sin t;  the backward pass turns the gradient by -t.  The
 // angle depends on the token and the pair only, so the 2 a heads of a token's Q and K share one table of n (cos, sin).
 //
-// Bound by HBM, and by the latency of a workgroup's life (loads, table, stores): 2/3 of the projection is read and written once, at up to
-// 6.1 TB/s (2048 tokens x 64 heads of 128 in bf16: 21.9 us).  A workgroup takes as many whole tokens as give its 256 threads U vectors each, or a part of one; it asks for its vectors first,
-// and makes the table in LDS while they are on their way.  U: 1 for 16-byte vectors of both halves in bf16, whose 32 registers a piece cost
-// waves, 3 otherwise (2048 tokens x 64 heads of 128: 29.0 | 32.6 us with 1 | 4; 4 x 1024 x 16 heads of 96, fp32: 22.0 | 20.1 | 21.3 with
-// 1 | 3 | 4, bf16 neighbours 14.2 | 10.0 | 10.5).  Angles are taken in turns
+// 2/3 of the projection is read and written once: bound by memory where it is large (2048 tokens x 64 heads of 128 in bf16: 21.4 us and 6.3 TB/s a
+// launch on the same tensors again, whose lines the memory-side cache holds in part, 27.6 on others), by the latency of a workgroup's life (loads,
+// table, stores) where it is small: waves wait 2/3 to 3/4 of their time (profiles/operators_counters.txt).
+// A workgroup takes as many whole tokens as give its 256 threads U vectors each, or a part of one; it asks for its vectors first, and makes the table in
+// LDS while they are on their way.  U: 1 for 16-byte vectors of both halves in bf16, whose 32 registers a piece cost waves, 3 otherwise.  Two launches,
+// there and back, over U: 2048 tokens x 64 heads of 128 58 | 65 us with 1 | 4; one: 4 x 1024 x 16 heads of 96, fp32 22.0 | 20.1 | 21.3 with 1 | 3 | 4,
+// bf16 neighbours 14.2 | 10.0 | 10.5.  Whole tokens leave places idle (288 vectors a token: 576 of 768).  Angles are taken in turns
 // (freq / 2 pi), in 64 bits, and reduced to [-1/2, 1/2] there: a float has no fraction left at position 10^6.  What a float loses of the reduced angle
 // is put back into its sine and cosine, or that error would be as large as their own rounding (cosines off by 3.4e-8 rms instead of 1.9e-8, in the same time).
 #include <cmath>
